@@ -458,10 +458,22 @@ def _vec(t, n, dev, what):
 
 
 def _stat(t, rows, cols, dev, what):
-    """Address of a contiguous fp32 matrix."""
-    if _mat(t, rows, cols, dev, what) != cols and t.numel():
+    """Address of a contiguous fp32 matrix (a single row is, whatever it is a slice of)."""
+    if _mat(t, rows, cols, dev, what) != cols and rows > 1 and t.numel():
         _refuse(t, (rows, cols), what)
     return t.data_ptr()
+
+
+def _stat_in(t, rows, cols, dev, what, stream):
+    """A statistic that is only read, as the library takes it: one whose rows or columns have gaps between
+    them (a slice, a transposed result) is copied first, on the call's stream."""
+    if t.dtype is torch.float32 and t.get_device() == dev and t.shape == (rows, cols) and not t.is_contiguous():
+        down, across = t.stride()
+        if (cols == 1 or across == 1) and (rows == 1 or down >= cols) or down == 1 and across >= rows:
+            with torch.cuda.device(dev), torch.cuda.stream(stream):
+                return t.contiguous()
+    _stat(t, rows, cols, dev, what)
+    return t
 
 
 def _device_of(t):
@@ -521,13 +533,16 @@ def group_norm(X, groups, gamma, beta, out, mean, rstd, seg_ptr=None, max_seg=-1
 def group_norm_bwd(X, dY, mean, rstd, groups, gamma, beta, dX=None, dgamma=None, dbeta=None, seg_ptr=None,
                    max_seg=-1, act=ACT_NONE, ws: _Workspace | None = None, stream=None):
     """Gradients of group_norm from dY = dLoss/dout, with the mean and rstd it wrote
-    (gcn_group_norm_bwd): dX (may be dY), dgamma, dbeta; each may be None."""
+    (gcn_group_norm_bwd): dX (may be dY), dgamma, dbeta; each may be None.  mean and rstd may have
+    rows or columns apart (slices, transposed results): such a one is copied first."""
     dev = _device_of(X)
     n, c = X.shape
     k, seg = _segments(seg_ptr, dev)
+    mean = _stat_in(mean, k, groups, dev, "mean", stream)
+    rstd = _stat_in(rstd, k, groups, dev, "rstd", stream)
     _call(_lib.gcn_group_norm_bwd,
           (n, c, groups, k, seg, max_seg, X.data_ptr(), _mat(X, n, c, dev, "X"), _vec(gamma, c, dev, "gamma"),
-           _vec(beta, c, dev, "beta"), act, _stat(mean, k, groups, dev, "mean"), _stat(rstd, k, groups, dev, "rstd"),
+           _vec(beta, c, dev, "beta"), act, mean.data_ptr(), rstd.data_ptr(),
            dY.data_ptr(), _mat(dY, n, c, dev, "dY"), _ptr(dX), _mat(dX, n, c, dev, "dX") if dX is not None else 0,
            _vec(dgamma, c, dev, "dgamma"), _vec(dbeta, c, dev, "dbeta")),
           "gcn_group_norm_bwd", ws, dev, stream)

@@ -1,0 +1,87 @@
+"""What the binding's norm calls take: statistics of any layout in the backward pass."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def G():
+    assert torch.cuda.is_available(), "GPU tests need a HIP device"
+    import paper_2512_01678_amd.gcn as G
+    return G
+
+
+def batch(n, c, k, seed):
+    rng = np.random.default_rng(seed)
+    ptr = [0, *np.sort(rng.integers(0, n + 1, k - 1)).tolist(), n]
+    dev = lambda *s: torch.from_numpy(rng.standard_normal(s).astype(np.float32)).cuda()
+    return dev(n, c), dev(n, c), dev(c), dev(c), torch.tensor(ptr, device="cuda")
+
+
+def layouts(v):
+    """The same values with rows or columns apart, and as a copy with none."""
+    k, g = v.shape
+    wide, tall = torch.full((k + 2, g + 3), 9.0, device="cuda"), torch.full((g + 1, k + 5), 9.0, device="cuda")
+    wide[1:k + 1, 2:g + 2] = v
+    tall[:g, 1:k + 1] = v.T
+    return dict(dense=v.clone(), turned=v.T.clone(memory_format=torch.contiguous_format).T, slice=wide[1:k + 1, 2:g + 2], turned_slice=tall[:g, 1:k + 1].T)
+
+
+@pytest.mark.parametrize("k,groups", [(1, 1), (1, 4), (5, 1), (5, 4), (300, 8)])
+def test_backward_takes_statistics_of_any_layout(G, k, groups):
+    x, dy, ga, be, seg = batch(900, 16, k, 1)
+    kw = dict(seg_ptr=seg, max_seg=900, act=G.ACT_SILU)
+    mean, rstd = torch.empty(k, groups, device="cuda"), torch.empty(k, groups, device="cuda")
+    G.group_norm(x, groups, ga, be, torch.empty_like(x), mean, rstd, **kw)
+
+    def run(mean, rstd, stream=None):
+        out = torch.zeros_like(x), torch.zeros_like(ga), torch.zeros_like(be)
+        torch.cuda.synchronize()
+        G.group_norm_bwd(x, dy, mean, rstd, groups, ga, be, *out, stream=stream, **kw)
+        torch.cuda.synchronize()
+        return out
+
+    want = run(mean, rstd)
+    means, rstds = layouts(mean), layouts(rstd)
+    for a in means:
+        for b in rstds:
+            for stream in (None, torch.cuda.Stream()):
+                for got, w in zip(run(means[a], rstds[b], stream), want):
+                    assert torch.equal(got, w), (a, b)
+    # captured: the copy is part of the graph, and takes the values of the time of the replay
+    out, turned = [torch.zeros_like(w) for w in want], [means["turned"], rstds["turned"]]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        G.group_norm_bwd(x, dy, *turned, groups, ga, be, *out, **kw)
+    for rep in range(3):
+        for t, v in zip(turned, (mean, rstd)):
+            t.copy_(v * (1 + rep))
+        expect = run(mean * (1 + rep), rstd * (1 + rep))
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, w in zip(out, expect):
+            assert torch.equal(got, w), rep
+
+
+def test_statistics_with_gaps_or_overlaps_are_refused(G):
+    x, dy, ga, be, seg = batch(40, 8, 3, 2)
+    z = lambda *s: torch.zeros(*s, device="cuda")
+    ok = z(3, 2)
+    for bad in (z(3, 4)[:, ::2], z(1, 2).expand(3, 2), z(3, 1).expand(3, 2), z(2, 3), z(4, 2), z(3, 2).double(),
+                z(3, 2).cpu(), z(6), z(3, 2, 1)):
+        for args in ((bad, ok), (ok, bad)):
+            with pytest.raises(ValueError):
+                G.group_norm_bwd(x, dy, *args, 2, ga, be, torch.zeros_like(x), seg_ptr=seg)
+    # what is written has to be dense; a row of a wider buffer is
+    for bad in (z(2, 3).T, z(3, 4)[:, :2]):
+        for args in ((bad, ok), (ok, bad)):
+            with pytest.raises(ValueError):
+                G.group_norm(x, 2, ga, be, torch.zeros_like(x), *args, seg_ptr=seg)
+    mean, rstd = z(5, 7)[2:3, 1:3], z(5, 7)[2:3, 1:3]
+    dense = z(1, 2), z(1, 2)
+    y, w = torch.zeros_like(x), torch.zeros_like(x)
+    G.group_norm(x, 2, ga, be, y, mean, rstd)
+    G.group_norm(x, 2, ga, be, w, *dense)
+    assert torch.equal(y, w) and torch.equal(mean, dense[0]) and torch.equal(rstd, dense[1])
