@@ -468,7 +468,9 @@ gcn_status gcn_column_sums(int64_t rows, int32_t w, const float* d_G, int64_t ld
  * empty graph); gcn_group_norm_bwd takes them.  d_Y: n x c (pitch ldy); it may be d_X
  * itself with the same pitch, and must not overlap it otherwise.  A group that holds an
  * infinity or NaN becomes NaN; the other groups and graphs do not see it.  Sums are held in
- * fp32 about a value of the group; the parts of a long graph are joined in fp64.
+ * fp32 about a value of the group; the parts of a long graph are joined in fp64.  mu is rounded
+ * once, when it is written, and y formed from it: a group whose values are all equal has that value
+ * as its mu, and y = act(beta_c), to the last bit.
  * Errors: GCN_E_INVALID (c % groups != 0; c, groups >= 1 and a finite eps >= 0 are needed),
  * GCN_E_OVERFLOW for more than 2^27 (graph, group) pairs, GCN_E_UNSUPPORTED for a pitch above
  * 2^20.

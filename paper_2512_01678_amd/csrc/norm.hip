@@ -22,20 +22,23 @@
 //
 // Precision: a thread sums (x - k) and (x - k)^2 about k, its first value, in fp32 (a
 // mean far from zero then costs no digits); threads and pieces are joined by their counts,
-// means and squared deviations (Chan, Golub, LeVeque 1979), pieces in fp64.
+// means and squared deviations (Chan, Golub, LeVeque 1979), the means as distances from a value
+// of the group, pieces in fp64.  The mean is rounded once, when it is written.
 #include "norm_device.h"
 
 namespace gcn {
 namespace {
 
-// Pass 1, forward: mean and squared deviations of every piece and fragment.
+// Pass 1, forward: a value close to the mean, distances and squared distances from it, of every piece and
+// fragment.
 template <int V>
 __global__ void __launch_bounds__(kThreads) k_norm_stats(NormArgs a) {
-  __shared__ float red[kThreads * V];
-  __shared__ float fmean[kThreads * V];
-  __shared__ float fdev[kThreads * V];
+  __shared__ JoinBox<V> box;
   const NormParams& p = a.p;
   const Place<V> t(a);
+  int32_t g[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) g[j] = (t.c0 + j < p.c ? t.c0 + j : p.c - 1) / a.cg;
   const int64_t r0 = (int64_t)blockIdx.x * a.rows;
   const int64_t r1 = r0 + a.rows < p.n ? r0 + a.rows : p.n;
   int64_t r = r0;
@@ -49,13 +52,14 @@ __global__ void __launch_bounds__(kThreads) k_norm_stats(NormArgs a) {
       continue;
     }
     met = 0;
-    float mean[V], m2[V];
-    const float cnt = read_stats(p, t, r, e - r, mean, m2);
-    join_threads(a, t, cnt, mean, m2, (float)(e - r), red, fmean, fdev);
+    float first[V], md[V], m2[V];
+    const float cnt = read_stats(p, t, r, e - r, first, md, m2);
+    join_threads(a, t, cnt, first, md, m2, g, (float)(e - r), box);
     const int64_t piece = ((int64_t)blockIdx.x + s) * a.n_frag + t.panel + t.gfirst;
     for (int f = threadIdx.x; f < t.nf; f += kThreads) {
-      a.part0[piece + f] = fmean[f];
-      a.part1[piece + f] = fdev[f];
+      a.part0[piece + f] = box.mean[f];
+      a.part1[piece + f] = box.dev[f];
+      a.part2[piece + f] = box.rest[f];
     }
     __syncthreads();
     r = e;
@@ -90,10 +94,11 @@ __device__ __forceinline__ Joined join_pieces(const NormArgs& a, int32_t s, int3
           v.s0 += (double)a.part0[at];
           v.s1 += (double)a.part1[at];
         } else {
-          // about the first piece's mean, in fp64
+          // about the first piece's value, in fp64
           const double m = (double)(re - rb) * (double)(hi - lo), d = (double)a.part0[at] - v.ref;
-          v.s0 += m * d;
-          v.s1 += (double)a.part1[at] + m * d * d;
+          const double rest = (double)a.part2[at];
+          v.s0 += m * d + rest;
+          v.s1 += (double)a.part1[at] + (m * d + 2.0 * rest) * d;
         }
       }
     }
@@ -431,6 +436,7 @@ NormArgs plan(const NormParams& p, bool bwd, bool vec, Arena& w) {
     const int64_t pieces = (a.n_block + p.n_seg) * a.n_frag;
     a.part0 = w.take<float>(pieces);
     a.part1 = w.take<float>(pieces);
+    if (!bwd) a.part2 = w.take<float>(pieces);
   }
   if (bwd) {
     if (!a.one) {

@@ -23,8 +23,9 @@ struct NormArgs {
   int one;          // threads per graph of the one-pass form, or 0
   int32_t n_col;    // workgroups of a panel that add column sums in the backward's second pass
   bool joined;      // one graph of few pieces: pass 2 joins them itself
-  float* part0;     // per piece and fragment: mean, or sum of gamma d
-  float* part1;     // squared deviations, or sum of gamma d xh
+  float* part0;     // per piece and fragment: a value close to the mean, or sum of gamma d
+  float* part1;     // squared distances from it, or sum of gamma d xh
+  float* part2;     // forward: distances from it
   float* m1;        // per (graph, group)
   float* m2;
   float* col0;      // per block and column: sum of d
@@ -262,11 +263,11 @@ __device__ __forceinline__ void frag_cols(const NormArgs& a, int32_t p0, int32_t
   hi = (e < pe ? e : pe) - p0;
 }
 
-// Sums over each fragment of red (ry rows of pw columns) in a fixed order; emit(f, sum) on one
+// Sums over each fragment of K arrays red (ry rows of pw columns each) in a fixed order; emit(f, sums) on one
 // lane each.  Lanes of a wavefront share a fragment: lc of them over its columns, the others over rows.
-template <int NT = kThreads, class Emit>
-__device__ __forceinline__ void frag_sums(const NormArgs& a, int32_t p0, int32_t gfirst, int nf, int ry,
-                                          const float* red, Emit emit) {
+template <int NT, int K, class Emit>
+__device__ __forceinline__ void frag_sums_of(const NormArgs& a, int32_t p0, int32_t gfirst, int nf, int ry,
+                                             const float* const (&red)[K], Emit emit) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int w = a.cg < a.pw ? a.cg : a.pw;
   int lc = 1;
@@ -277,47 +278,81 @@ __device__ __forceinline__ void frag_sums(const NormArgs& a, int32_t p0, int32_t
   const int sub = lane & (lc * lr - 1);
   for (int f0 = wave * per; f0 < nf; f0 += (NT / 64) * per) {
     const int f = f0 + lane / (lc * lr);
-    float v = 0.f;
+    float v[K] = {};
     if (f < nf) {
       int lo, hi;
       frag_cols(a, p0, gfirst, f, lo, hi);
       for (int y = sub / lc; y < ry; y += lr)
-        for (int c = lo + (sub & (lc - 1)); c < hi; c += lc) v += red[y * a.pw + c];
+        for (int c = lo + (sub & (lc - 1)); c < hi; c += lc)
+#pragma unroll
+          for (int k = 0; k < K; ++k) v[k] += red[k][y * a.pw + c];
     }
-    for (int o = (lc * lr) >> 1; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    for (int o = (lc * lr) >> 1; o > 0; o >>= 1)
+#pragma unroll
+      for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], o, 64);
     if (f < nf && sub == 0) emit(f, v);
   }
 }
+template <int NT = kThreads, class Emit>
+__device__ __forceinline__ void frag_sums(const NormArgs& a, int32_t p0, int32_t gfirst, int nf, int ry,
+                                          const float* red, Emit emit) {
+  const float* const one[1] = {red};
+  frag_sums_of<NT, 1>(a, p0, gfirst, nf, ry, one, [&](int f, const float* v) { emit(f, v[0]); });
+}
 
-// A thread's values as count, means and squared deviations, joined: fmean[f] and fdev[f] of the panel's
-// fragments over `rows` rows, in LDS, for all threads behind the call.
+// LDS of join_threads: a panel has at most 64 V columns.
+template <int V>
+struct JoinBox {
+  float red0[kThreads * V], red1[kThreads * V];
+  float mean[64 * V], rest[64 * V], dev[64 * V];
+};
+
+// The threads' values joined over `rows` rows: box.mean[f] is a value close to the mean of the panel's fragment f,
+// box.rest[f] and box.dev[f] the sums of the distances and of the squared distances from it, for all threads behind the
+// call.  A thread has cnt values, first among them, of mean first + md and squared deviations m2.  What is added up
+// is distances, from a value of the fragment (that of its first column in the first row, which has values) and then
+// from the mean that this gives: differences of values that are close are exact, so the size of the values costs no
+// digits, the rounding of the mean to fp32 is known (rest), and a constant group has exactly its value.
 template <int V, int NT>
-__device__ __forceinline__ void join_threads(const NormArgs& a, const Place<V, NT>& t, float cnt, const float* mean,
-                                             const float* m2, float rows, float* red, float* fmean, float* fdev) {
+__device__ __forceinline__ void join_threads(const NormArgs& a, const Place<V, NT>& t, float cnt, const float* first,
+                                             const float* md, const float* m2, const int32_t* g, float rows,
+                                             JoinBox<V>& box) {
+  if (t.ty == 0)
 #pragma unroll
-  for (int j = 0; j < V; ++j) red[t.ty * a.pw + t.tx * V + j] = cnt * mean[j];
+    for (int j = 0; j < V; ++j) box.rest[t.tx * V + j] = first[j];
   __syncthreads();
-  frag_sums<NT>(a, t.p0, t.gfirst, t.nf, t.ry, red, [&](int f, float v) {
+  const int at = t.ty * a.pw + t.tx * V;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const int32_t b = g[j] * a.cg;
+    box.red0[at + j] = cnt * ((first[j] - box.rest[(b > t.p0 ? b : t.p0) - t.p0]) + md[j]);
+  }
+  __syncthreads();
+  frag_sums<NT>(a, t.p0, t.gfirst, t.nf, t.ry, box.red0, [&](int f, float v) {
     int lo, hi;
     frag_cols(a, t.p0, t.gfirst, f, lo, hi);
-    fmean[f] = v / (rows * (float)(hi - lo));
+    box.mean[f] = box.rest[lo] + v / (rows * (float)(hi - lo));
   });
   __syncthreads();
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const int32_t c = t.c0 + j;
-    const float d = c < a.p.c ? mean[j] - fmean[c / a.cg - t.gfirst] : 0.f;
-    red[t.ty * a.pw + t.tx * V + j] = m2[j] + cnt * d * d;
+    const float d = (first[j] - box.mean[g[j] - t.gfirst]) + md[j];
+    box.red0[at + j] = cnt * d;
+    box.red1[at + j] = m2[j] + cnt * d * d;
   }
   __syncthreads();
-  frag_sums<NT>(a, t.p0, t.gfirst, t.nf, t.ry, red, [&](int f, float v) { fdev[f] = v; });
+  const float* const both[2] = {box.red0, box.red1};
+  frag_sums_of<NT, 2>(a, t.p0, t.gfirst, t.nf, t.ry, both, [&](int f, const float* v) {
+    box.rest[f] = v[0];
+    box.dev[f] = v[1];
+  });
   __syncthreads();
 }
 
-// Count, means and squared deviations of this thread's rows among [r, r + len).
+// Count, first value, mean less that and squared deviations of this thread's rows among [r, r + len).
 template <int V, int NT>
 __device__ __forceinline__ float read_stats(const NormParams& p, const Place<V, NT>& t, int64_t r, int64_t len,
-                                            float* mean, float* m2) {
+                                            float* first, float* md, float* m2) {
   Vals<V> k{}, sum{}, sq{};
   float cnt = 0.f;
   if (t.left > 0 && t.ty < len) {
@@ -337,11 +372,19 @@ __device__ __forceinline__ float read_stats(const NormParams& p, const Place<V, 
   const float inv = cnt > 0.f ? 1.f / cnt : 0.f;
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const float md = sum.v[j] * inv;
-    mean[j] = k.v[j] + md;
-    m2[j] = sq.v[j] - sum.v[j] * md;
+    first[j] = k.v[j];
+    md[j] = sum.v[j] * inv;
+    m2[j] = sq.v[j] - sum.v[j] * md[j];
   }
   return cnt;
+}
+
+// Mean and 1 / sqrt(var + eps) of 1 / inv elements from what join_threads leaves of their group.
+__device__ __forceinline__ void finish_stats(float center, float rest, float dev, double inv, double eps, float& mean,
+                                             float& rstd) {
+  const double e = (double)rest * inv, var = (double)dev * inv - e * e;
+  mean = (float)((double)center + e);
+  rstd = (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + eps));
 }
 
 // The columns of a workgroup's panel: tot over its row lanes (red0, red1: as large as the workgroup).

@@ -9,9 +9,7 @@ namespace {
 // time; a graph of more of them is read again for the result.
 template <int V, int ACT>
 __global__ void __launch_bounds__(kThreads) k_norm_one(NormArgs a) {
-  __shared__ float red[kThreads * V];
-  __shared__ float fmean[kThreads * V];
-  __shared__ float fdev[kThreads * V];
+  __shared__ JoinBox<V> box;
   constexpr int kRows = rows_fwd(kThreads);
   const NormParams& p = a.p;
   const int32_t s = blockIdx.x;
@@ -33,7 +31,7 @@ __global__ void __launch_bounds__(kThreads) k_norm_one(NormArgs a) {
   const float* src = p.X + b * p.ldx;
   const uint32_t off = t.off(p.ldx);
   Vals<V> x[kRows], first{};
-  float mean[V], m2[V], sum[V] = {}, sq[V] = {};
+  float sum[V] = {}, sq[V] = {};
   int64_t at = 0;
   auto load = [&]() {
     const float* row = src + at * p.ldx;
@@ -66,23 +64,23 @@ __global__ void __launch_bounds__(kThreads) k_norm_one(NormArgs a) {
   const float cnt = live ? (float)((len - t.ty + t.ry - 1) >> (8 - a.tx_log)) : 0.f, inv = live ? 1.f / cnt : 0.f;
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    mean[j] = first.v[j] + sum[j] * inv;
-    m2[j] = sq[j] - sum[j] * (sum[j] * inv);
+    sum[j] *= inv;
+    sq[j] -= sum[j] * (sum[j] * cnt);
   }
-  join_threads(a, t, cnt, mean, m2, (float)len, red, fmean, fdev);
+  join_threads(a, t, cnt, first.v, sum, sq, g, (float)len, box);
+  const double share = 1.0 / ((double)len * (double)a.cg);
   for (int f = threadIdx.x; f < t.nf; f += kThreads) {
-    const float r = (float)(1.0 / sqrt((double)fdev[f] / ((double)len * (double)a.cg) + p.eps));
-    fdev[f] = r;
-    p.mean[(int64_t)s * p.groups + t.gfirst + f] = fmean[f];
-    p.rstd[(int64_t)s * p.groups + t.gfirst + f] = r;
+    finish_stats(box.mean[f], box.rest[f], box.dev[f], share, p.eps, box.mean[f], box.dev[f]);
+    p.mean[(int64_t)s * p.groups + t.gfirst + f] = box.mean[f];
+    p.rstd[(int64_t)s * p.groups + t.gfirst + f] = box.dev[f];
   }
   __syncthreads();
   if (t.left <= 0) return;
-  float sc[V];
+  float mean[V], sc[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    mean[j] = fmean[g[j] - t.gfirst];
-    sc[j] = fdev[g[j] - t.gfirst];
+    mean[j] = box.mean[g[j] - t.gfirst];
+    sc[j] = box.dev[g[j] - t.gfirst];
   }
   const uint32_t off_y = t.off(p.ldy);
   for (;;) {
@@ -302,45 +300,44 @@ __global__ void __launch_bounds__(64) k_norm_wave(NormArgs a) {
     if (at + held >= len) break;
   }
   if (live) cnt = (float)((len - t.ty + t.ry - 1) >> (6 - a.tx_log));
-  // joined by counts, means and squared deviations (join_threads).  The means are joined as distances from one
-  // value of the group, so that a constant group has exactly its value, and then from the mean found, which
-  // takes the first join's rounding (that value may be far out) away again.
+  // joined as in join_threads: distances from one value of the group, and then from the mean that this gives
   const float inv = cnt > 0.f ? 1.f / cnt : 0.f, all = 1.f / fmaxf((float)len * (float)a.cg, 1.f);
-  float mean[4], fm[4], dev[4], from[4];
+  float center[4], rest[4], dev[4];
 #pragma unroll
   for (int k = 0; k < SUB; ++k) {
     const float v = __shfl(first.v[k * 4 / SUB], t.tx & ~(t.group_lanes - 1), 64);
 #pragma unroll
-    for (int j = 0; j < 4 / SUB; ++j) from[k * 4 / SUB + j] = v;
+    for (int j = 0; j < 4 / SUB; ++j) center[k * 4 / SUB + j] = v;
   }
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    mean[j] = first.v[j] + sum[j] * inv;
-    fm[j] = cnt * (mean[j] - from[j]);
+    sum[j] *= inv;
+    rest[j] = cnt * ((first.v[j] - center[j]) + sum[j]);
   }
-  t.sums(fm);
+  t.sums(rest);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    from[j] += fm[j] * all;
-    fm[j] = cnt * (mean[j] - from[j]);
+    center[j] += rest[j] * all;
+    const float d = (first.v[j] - center[j]) + sum[j];
+    rest[j] = cnt * d;
+    dev[j] = sq[j] - sum[j] * (sum[j] * cnt) + cnt * d * d;
   }
-  t.sums(fm);
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    fm[j] = from[j] + fm[j] * all;
-    const float d = mean[j] - fm[j];
-    dev[j] = sq[j] - sum[j] * (sum[j] * inv) + cnt * d * d;
-  }
+  t.sums(rest);
   t.sums(dev);
-  float sc[4];
+  float fm[4], sc[4];
+  const double share = 1.0 / ((double)len * (double)a.cg);
 #pragma unroll
   for (int k = 0; k < SUB; ++k) {
-    const float r = len > 0 ? (float)(1.0 / sqrt((double)(dev[k * 4 / SUB] * all) + p.eps)) : 0.f;
+    float m = 0.f, r = 0.f;
+    if (len > 0) finish_stats(center[k * 4 / SUB], rest[k * 4 / SUB], dev[k * 4 / SUB], share, p.eps, m, r);
 #pragma unroll
-    for (int j = 0; j < 4 / SUB; ++j) sc[k * 4 / SUB + j] = r;
+    for (int j = 0; j < 4 / SUB; ++j) {
+      fm[k * 4 / SUB + j] = m;
+      sc[k * 4 / SUB + j] = r;
+    }
     // the first lane of the group in the first row
     if (t.left > k * 4 / SUB && t.ty == 0 && (t.tx & (t.group_lanes - 1)) == 0) {
-      p.mean[s * p.groups + g[k * 4 / SUB]] = len > 0 ? fm[k * 4 / SUB] : 0.f;
+      p.mean[s * p.groups + g[k * 4 / SUB]] = m;
       p.rstd[s * p.groups + g[k * 4 / SUB]] = r;
     }
   }
