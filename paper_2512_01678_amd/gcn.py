@@ -168,23 +168,64 @@ def _ld(t):
 
 
 class _Workspace:
+    """Device scratch that is kept from call to call and grows to the largest size asked for.
+
+    A buffer serves the stream that it was allocated on.  A call on another stream gets one of its own in its
+    place: calls on two streams share no scratch, and what is freed goes back to the only stream that used it.
+    A call that is captured into a graph takes what is there, and a buffer that a graph uses is kept as long as
+    the workspace: keep that as long as the graph, and run what shares it (replays of its graphs, calls) one
+    after the other."""
+
     def __init__(self):
         self.buf = None
+        self.stream = None  # handle of the stream that buf belongs to
+        self.held = []      # buffers that a graph uses
 
-    def get(self, nbytes, device):
+    def hold(self):
+        if not any(b is self.buf for b in self.held):
+            self.held.append(self.buf)
+
+    def kept(self, nbytes, dev, stream, capturing):
+        """The buffer, if it is large enough and a call on this stream of device `dev` may use it."""
+        buf = self.buf
+        if buf is None or buf.get_device() != dev or buf.numel() < nbytes:
+            return None
+        if capturing:
+            self.hold()
+        elif stream != self.stream:
+            return None
+        return buf
+
+    def take(self, nbytes, dev, stream, capturing):
+        """The buffer for a call on `stream`, the current one (dev -1: in host memory)."""
+        if self.kept(nbytes, dev, stream, capturing) is None:
+            self.buf = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=dev if dev >= 0 else "cpu")
+            self.stream = stream
+            if capturing:
+                self.hold()
+        return self.buf
+
+    def get(self, nbytes, device, stream=None):
+        """The same for a call on the stream of this handle (None: the current one)."""
         if nbytes == 0:
             return None
-        if self.buf is None or self.buf.numel() < nbytes or self.buf.device != torch.device(device):
-            self.buf = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
-        return self.buf
+        device = torch.device(device)
+        dev = device.index if device.index is not None else torch.cuda.current_device()
+        current = torch.cuda.current_stream(dev).cuda_stream
+        if stream is None or stream == current:
+            return self.take(nbytes, dev, current, torch.cuda.is_current_stream_capturing())
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream, dev) if stream else torch.cuda.default_stream(dev)):
+            return self.take(nbytes, dev, stream, torch.cuda.is_current_stream_capturing())
 
 
 def _run_ws(fn, args_before, args_after, where, ws: _Workspace | None, device):
-    """Two-phase workspace protocol: size query, then the call with a buffer that large."""
+    """Two-phase workspace protocol: size query, then the call with a buffer that large.  args_after begins with the
+    handle of the call's stream."""
     nbytes = sz(0)
     _check(fn(*args_before, None, C.byref(nbytes), *args_after), where + " (size query)")
     ws = ws or _Workspace()
-    buf = ws.get(max(nbytes.value, 256), device)
+    stream = args_after[0]
+    buf = ws.get(max(nbytes.value, 256), device, (stream.value or 0) if isinstance(stream, P) else stream)
     nbytes = sz(buf.numel())
     _check(fn(*args_before, buf.data_ptr(), C.byref(nbytes), *args_after), where)
     return ws
@@ -485,23 +526,24 @@ def _device_of(t):
 def _call(fn, args, where, ws, dev, stream):
     """fn(*args, workspace, its size, stream) with device `dev` current, on `stream` or that device's
     current one.  A workspace kept in ws is tried first; its size is asked for only if it is too small."""
+    if stream is not None and stream.device.index != dev:
+        raise ValueError(f"{where}: a stream of the tensors' device needed")
     if dev != torch.cuda.current_device():
         with torch.cuda.device(dev):
             return _call(fn, args, where, ws, dev, stream)
-    st = (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
-    buf = ws.buf if ws is not None else None
-    if buf is not None and buf.get_device() == dev:
+    st = torch.cuda.current_stream().cuda_stream
+    if stream is not None and stream.cuda_stream != st:
+        with torch.cuda.stream(stream):
+            return _call(fn, args, where, ws, dev, None)
+    buf = ws.kept(0, dev, st, torch.cuda.is_current_stream_capturing()) if ws is not None else None
+    if buf is not None:
         nbytes = sz(buf.numel())
         status = fn(*args, buf.data_ptr(), C.byref(nbytes), st)
         if status == OK:
             return
         if status != E_CAPACITY:
             _check(status, where)
-    if stream is None:
-        _run_ws(fn, args, (st,), where, ws, torch.device("cuda", dev))
-    else:
-        with torch.cuda.stream(stream):  # a buffer of that stream: freed, it is not used again before the call is done
-            _run_ws(fn, args, (st,), where, ws, torch.device("cuda", dev))
+    _run_ws(fn, args, (st,), where, ws, torch.device("cuda", dev))
 
 
 def _segments(seg_ptr, dev):
@@ -710,6 +752,7 @@ class Model:
     def epoch_captured(self, g: DeviceGraph, X=None, x: SparseFeatures | None = None, labels=None):
         """Enqueue one epoch with the prepared workspace and no allocation (for HIP graph capture)."""
         buf = self._ws.buf
+        self._ws.hold()
         nbytes = sz(buf.numel())
         _check(_lib.gcn_epoch(C.byref(self.c), C.byref(g.c), _ptr(X), C.byref(x.c) if x is not None else None,
                               _ptr(labels), _ptr(self.loss), buf.data_ptr(), C.byref(nbytes),

@@ -1,4 +1,5 @@
-"""What the binding's norm calls take: statistics of any layout in the backward pass."""
+"""What the binding's calls take: statistics of any layout in the backward pass, and a workspace that goes from
+stream to stream and into graphs."""
 import numpy as np
 import pytest
 import torch
@@ -85,3 +86,64 @@ def test_statistics_with_gaps_or_overlaps_are_refused(G):
     G.group_norm(x, 2, ga, be, y, mean, rstd)
     G.group_norm(x, 2, ga, be, w, *dense)
     assert torch.equal(y, w) and torch.equal(mean, dense[0]) and torch.equal(rstd, dense[1])
+
+
+def test_a_workspace_that_goes_from_stream_to_stream(G):
+    """Calls on two streams in turn, growing, with other work of both streams beside them: every result as alone."""
+    cases = [(3000 + 40000 * i, 64, 1 + 3 * i) for i in range(4)]
+    data = [batch(n, c, k, i) for i, (n, c, k) in enumerate(cases)]
+
+    def buffers(n, c, k):
+        z = lambda *s: torch.zeros(*s, device="cuda")
+        return z(n, c), z(k, 8), z(k, 8), z(n, c), z(c), z(c)
+
+    def run(i, o, ws, stream=None):
+        x, dy, ga, be, seg = data[i]
+        kw = dict(seg_ptr=seg, act=G.ACT_SILU, ws=ws, stream=stream)
+        G.group_norm(x, 8, ga, be, o[0], o[1], o[2], **kw)
+        G.group_norm_bwd(x, dy, o[1], o[2], 8, ga, be, o[3], o[4], o[5], **kw)
+
+    want = [buffers(*c) for c in cases]
+    for i in range(4):
+        run(i, want[i], None)
+    work = torch.ones(1 << 26, device="cuda")
+    streams = [None, torch.cuda.Stream(), torch.cuda.Stream()]
+    for turn in range(3):
+        got, ws = [buffers(*c) for c in cases], G._Workspace()
+        torch.cuda.synchronize()
+        for i in range(4):
+            s = streams[(turn + i) % 3]
+            with torch.cuda.stream(s):
+                for _ in range(5):
+                    work.mul_(1.0) if s is None else torch.ones(1 << 24, device="cuda")
+            run(i, got[i], ws, s)
+            junk = [torch.full((v,), float("nan"), device="cuda") for v in (1 << 12, 1 << 16, 1 << 20) for _ in range(20)]
+            assert junk
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            for a, b in zip(g, w):
+                assert torch.equal(a, b), turn
+
+
+def test_a_graph_keeps_its_scratch_when_the_workspace_grows(G):
+    x, dy, ga, be, seg = batch(50000, 64, 9, 1)
+    z = lambda *s: torch.zeros(*s, device="cuda")
+    y, mean, rstd, ws = z(50000, 64), z(9, 8), z(9, 8), G._Workspace()
+    kw = dict(seg_ptr=seg, act=G.ACT_SILU)
+    G.group_norm(x, 8, ga, be, y, mean, rstd, ws=ws, **kw)
+    want, small = y.clone(), ws.buf
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        G.group_norm(x, 8, ga, be, y, mean, rstd, ws=ws, **kw)
+    big = torch.randn(700, 700, device="cuda")
+    G.orthogonalize(big, torch.empty_like(big), ws=ws)
+    assert ws.buf is not small and any(b is small for b in ws.held)
+    at = small.data_ptr()
+    del small
+    for rep in range(3):
+        junk = [torch.full((v,), float("nan"), device="cuda") for v in (1 << 12, 1 << 16, 1 << 20) for _ in range(20)]
+        assert all(t.data_ptr() != at for t in junk)
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want), rep
