@@ -41,6 +41,7 @@ class GcnError(RuntimeError):
 
 
 SPLIT_MIN, SPLIT_CHUNK = 4096, 2048
+MUON_MAX = 16  # matrices of a gcn_muon call
 
 
 class gcn_split(C.Structure):
@@ -612,7 +613,8 @@ def muon(params, grads, ms, lr=0.02, momentum=0.95, nesterov=True, weight_decay=
          ws: _Workspace | None = None, stream=None):
     """One optimiser step with orthogonalised updates over weight matrices, in place (gcn_muon);
     ms: momentum buffers (zero at first).  scales: what multiplies lr for each matrix, by default
-    sqrt(max(1, cols / rows)), the root of a layer's fan-out over its fan-in."""
+    sqrt(max(1, cols / rows)), the root of a layer's fan-out over its fan-in.  Any number of matrices: 16 share
+    the launches of a call, and all are checked before the first."""
     if not params:
         return
     if not len(params) == len(grads) == len(ms) or (scales is not None and len(scales) != len(params)):
@@ -629,8 +631,19 @@ def muon(params, grads, ms, lr=0.02, momentum=0.95, nesterov=True, weight_decay=
         t.m = _stat(m, rows, cols, dev, "m")
         t.rows, t.cols = rows, cols
         t.scale = scales[i] if scales is not None else max(1.0, cols / max(rows, 1)) ** 0.5
-    _call(_lib.gcn_muon, (arr, len(params), steps, lr, momentum, int(nesterov), weight_decay), "gcn_muon", ws, dev,
-          stream)
+    how = (steps, lr, momentum, int(nesterov), weight_decay)
+    size = C.sizeof(gcn_muon_tensor)
+    calls = [((gcn_muon_tensor * min(MUON_MAX, len(arr) - i)).from_buffer(arr, i * size), min(MUON_MAX, len(arr) - i))
+             for i in range(0, len(arr), MUON_MAX)]
+    if len(calls) > 1:
+        used = [t for t in arr if t.rows * t.cols]
+        written = [a for t in used for a in (t.param, t.m)]
+        if len(set(written)) < len(written) or not set(written).isdisjoint(t.grad for t in used):
+            raise ValueError("muon: a buffer that is written is given twice")
+        for some in calls:
+            _check(_lib.gcn_muon(*some, *how, None, C.byref(sz(0)), None), "gcn_muon (size query)")
+    for some in calls:
+        _call(_lib.gcn_muon, (*some, *how), "gcn_muon", ws, dev, stream)
 
 
 def layer_order(f_in, f_out, index, act, x_sparse=False, order=ORDER_AUTO, agg=AGG_NORM):
