@@ -561,7 +561,8 @@ typedef struct gcn_muon_tensor {
  * twice).  Workspace, with the sides of a matrix padded to 64:
  * 12 bytes per element, 8 per element of the shorter side's square, and for the parts of a sum
  * over the longer side up to 40 MB in all, or 2 bytes per element of that square for each 1,024 of it;
- * none where all matrices are at most 32 x 1,536 or 64 x 768.
+ * none where, over all matrices of the call, the shorter sides are at most 32 and the longer ones at most 1,536, or
+ * the shorter ones at most 64 and the longer ones at most 768.
  */
 gcn_status gcn_muon(const gcn_muon_tensor* t, int32_t count, int32_t steps, double lr, double momentum,
                     int32_t nesterov, double weight_decay, void* d_ws, size_t* ws_bytes, hipStream_t stream);
