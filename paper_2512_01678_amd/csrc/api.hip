@@ -909,7 +909,7 @@ gcn_status gcn_group_norm_fwd(int64_t n, int32_t c, int32_t groups, int32_t n_se
   if (query) return GCN_OK;
   if ((n_seg > 0 && (!d_mean || !d_rstd)) || (n > 0 && n_seg > 0 && (!d_X || !d_Y)))
     return fail(GCN_E_INVALID, "gcn_group_norm_fwd: NULL buffer");
-  if (d_X == d_Y && ldx != ldy) return fail(GCN_E_INVALID, "gcn_group_norm_fwd: in place takes one pitch");
+  if (n > 0 && d_X == d_Y && ldx != ldy) return fail(GCN_E_INVALID, "gcn_group_norm_fwd: in place takes one pitch");
   return launch_group_norm(p, d_ws, stream);
 }
 
@@ -938,7 +938,7 @@ gcn_status gcn_group_norm_bwd(int64_t n, int32_t c, int32_t groups, int32_t n_se
   if (query) return GCN_OK;
   if ((n_seg > 0 && (!d_mean || !d_rstd)) || (n > 0 && n_seg > 0 && (!d_X || !d_dY)))
     return fail(GCN_E_INVALID, "gcn_group_norm_bwd: NULL buffer");
-  if (d_dX && ((d_dX == d_dY && lddx != lddy) || d_dX == d_X))
+  if (n > 0 && d_dX && ((d_dX == d_dY && lddx != lddy) || d_dX == d_X))
     return fail(GCN_E_INVALID, "gcn_group_norm_bwd: d_dX may be d_dY (one pitch), not d_X");
   return launch_group_norm_bwd(p, d_ws, stream);
 }
@@ -973,7 +973,8 @@ gcn_status gcn_orthogonalize(int64_t rows, int64_t cols, const float* d_G, int64
   GCN_TRY(ws_protocol(d_ws, ws_bytes, newton_schulz_workspace(&t, 1), "gcn_orthogonalize", &query));
   if (query) return GCN_OK;
   if (rows > 0 && cols > 0 && (!d_G || !d_O)) return fail(GCN_E_INVALID, "gcn_orthogonalize: NULL buffer");
-  if (d_G == d_O && ldg != ldo) return fail(GCN_E_INVALID, "gcn_orthogonalize: in place takes one pitch");
+  if (rows > 0 && cols > 0 && d_G == d_O && ldg != ldo)
+    return fail(GCN_E_INVALID, "gcn_orthogonalize: in place takes one pitch");
   return launch_newton_schulz(&t, 1, steps, 0.0, false, 1.0, d_ws, stream);
 }
 
