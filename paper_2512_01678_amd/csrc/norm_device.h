@@ -209,12 +209,14 @@ __device__ __forceinline__ float activate(float z) {
   return z;
 }
 // act'(z) times dy; ReLU's derivative is 1[z > 0], as in the layers.  SiLU's is q (1 + z (1 - q)) with
-// q = 1 / (1 + e), 1 - q = e q; below z = -80, where it is less than 1e-32, e stays finite.
+// q = 1 / (1 + e), 1 - q = e q; below z = -80, where it is less than 1e-32, that of -80 is taken: e stays finite, and
+// q, which no longer falls, is not multiplied by a z that does.
 template <int ACT>
 __device__ __forceinline__ float act_grad(float dy, float z) {
   if constexpr (ACT == GCN_ACT_RELU) return z > 0.f ? dy : 0.f;
   if constexpr (ACT == GCN_ACT_SILU) {
-    const float e = exp_neg(z < -80.f ? -80.f : z), q = __builtin_amdgcn_rcpf(1.f + e);
+    z = z < -80.f ? -80.f : z;
+    const float e = exp_neg(z), q = __builtin_amdgcn_rcpf(1.f + e);
     return dy * (q * (1.f + z * (e * q)));
   }
   return dy;
