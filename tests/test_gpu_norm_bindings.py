@@ -147,3 +147,36 @@ def test_a_graph_keeps_its_scratch_when_the_workspace_grows(G):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, want), rep
+
+
+def test_the_other_calls_on_another_stream(G):
+    """Products and column sums, with a workspace that goes from stream to stream and with none: the scratch is the
+    stream's own, and what the current stream allocates meanwhile is other memory."""
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    a, b = torch.randn(20000, 64, device="cuda", generator=gen), torch.randn(20000, 48, device="cuda", generator=gen)
+    want, sums = torch.zeros(64, 48, device="cuda"), torch.zeros(64, device="cuda")
+    G.gemm(G.OP_TN, a, b, want)
+    G.column_sums(a, sums)
+    side, work = torch.cuda.Stream(), torch.ones(1 << 26, device="cuda")
+    for ws in (None, G._Workspace()):
+        for stream in (None, side, None, torch.cuda.default_stream(), side):
+            got, got_sums = torch.zeros_like(want), torch.zeros_like(sums)
+            torch.cuda.synchronize()
+            with torch.cuda.stream(stream):
+                for _ in range(5):
+                    work.mul_(1.0)
+            G.gemm(G.OP_TN, a, b, got, ws=ws, stream=stream)
+            G.column_sums(a, got_sums, stream=stream)
+            junk = [torch.full((v,), float("nan"), device="cuda") for v in (1 << 12, 1 << 16, 1 << 20) for _ in range(20)]
+            assert junk
+            if ws is not None:
+                assert ws.stream == (side if stream is side else torch.cuda.default_stream()).cuda_stream
+            torch.cuda.synchronize()
+            assert torch.equal(got, want) and torch.equal(got_sums, sums)
+    # the call on the default stream, while another is current
+    with torch.cuda.stream(side):
+        got = torch.zeros_like(want)
+        torch.cuda.synchronize()
+        G.gemm(G.OP_TN, a, b, got, ws=ws, stream=torch.cuda.default_stream())
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and ws.stream == torch.cuda.default_stream().cuda_stream
