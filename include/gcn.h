@@ -457,11 +457,12 @@ gcn_status gcn_column_sums(int64_t rows, int32_t w, const float* d_G, int64_t ld
  * offsets, graph s being rows [d_seg_ptr[s], d_seg_ptr[s+1]) (an empty graph is allowed);
  * offsets are taken as if cut to [0, n], and rows before the first graph and behind the
  * last are neither read nor written.  NULL: one graph of all n rows (n_seg must be 1).
- * max_seg: rows of the longest graph as known to the host, used only to shape the launch
- * (-1 if unknown; a wrong value costs time, not results).  The channels are cut into
- * `groups` equal groups (c % groups == 0): groups == c normalises every channel by itself,
- * groups == 1 the whole graph.  With N the elements of one (graph, group), mu = sum x / N,
- * var = sum (x - mu)^2 / N, r = 1 / sqrt(var + eps):
+ * max_seg: rows of the longest graph as known to the host, used only to shape the launch.  -1 if
+ * unknown: batches of small graphs are then read twice, which takes up to twice the time.  A
+ * wrong value costs time, and makes longer chains of fp32 additions of the sums of a graph that
+ * is many times longer.  The channels are cut into `groups` equal groups (c % groups == 0):
+ * groups == c normalises every channel by itself, groups == 1 the whole graph.  With N the
+ * elements of one (graph, group), mu = sum x / N, var = sum (x - mu)^2 / N, r = 1 / sqrt(var + eps):
  *   y = act(gamma_c (x - mu) r + beta_c)
  * d_gamma, d_beta: c each, or NULL (1 and 0).  act: GCN_ACT_NONE, GCN_ACT_RELU (NaN stays
  * NaN) or GCN_ACT_SILU.  d_mean, d_rstd: n_seg x groups, receive mu and r (both 0 for an

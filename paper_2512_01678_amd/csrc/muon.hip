@@ -14,10 +14,11 @@
 // Arithmetic: matrices here are bounded (singular values stay below 1.3), so a value v is held as
 // two fp16 parts of v 2^s: hi the nearest fp16, lo the nearest fp16 of the rest.  Together they
 // keep 22 bits and a sign, an error of at most 2^-23 relative, and a product is three matrix
-// instructions, hi hi + hi lo + lo hi, accumulated in fp32 (lo lo is below 2^-24 of the product):
-// half of the six that the exact split into bf16 parts (bf16x6.h) takes at twice the speed of
-// light.  The scales (2^12 for X, 2^10 for A and B) keep hi of any element that matters out of
-// fp16's subnormal range and the largest below 2^13.
+// instructions, hi hi + hi lo + lo hi, accumulated in fp32 (lo lo is at most 2^-22 of the product
+// and 2^-25 of it on average, which leaves the error of the whole at that of fp32 products): half
+// of the six that the exact split into bf16 parts (bf16x6.h) takes at twice the speed of light.
+// The scales (2^12 for X, 2^10 for A and B) keep hi of any element that matters out of fp16's
+// subnormal range and the largest below 2^13.
 #include <hip/hip_fp16.h>
 
 #include <type_traits>

@@ -385,13 +385,13 @@ NormArgs plan(const NormParams& p, bool bwd, bool vec, Arena& w) {
   // call, is at most 16 times that.  Forward a wavefront a graph, where they fit that and the others of the batch
   // hide the longest.  128 channels, SiLU, lengths spread exponentially, one input again and again, microseconds:
   //   graphs x mean rows   wavefronts   workgroups   two passes   backward   in two passes
-  //        256 x 32            26           14           32          23           33
-  //        256 x 96            71           26           31          50           35
-  //       1024 x 32            28           19           45          31           48
-  //       1024 x 96            78           35           54          66           70
-  //       4096 x 32            43           50           90          68          109
-  //       4096 x 64            86           63          113         133          161
-  //       8192 x 32            71           88          150         136          196
+  //        256 x 32            30           15           33          23           33
+  //        256 x 96            82           29           31          50           35
+  //       1024 x 32            32           18           45          31           48
+  //       1024 x 96            93           36           59          66           70
+  //       4096 x 32            44           47           89          68          109
+  //       4096 x 64            89           62          112         133          161
+  //       8192 x 32            76           86          144         136          196
   // (A launch takes less than 2^32 threads.)
   if (p.seg_ptr && p.max_seg >= 0 && p.n_seg < (1 << 24) && (int64_t)p.n_seg * a.n_panel >= 256 &&
       (a.n_panel == 1 || a.pw % a.cg == 0)) {

@@ -561,7 +561,9 @@ def group_norm(X, groups, gamma, beta, out, mean, rstd, seg_ptr=None, max_seg=-1
     """out = act(gamma (X - mean) rstd + beta) per graph and channel group (gcn_group_norm_fwd).
 
     X, out: n x c (out may be X).  seg_ptr: int64 device offsets of the batch's graphs (None: one
-    graph); mean, rstd: (graphs, groups), written for group_norm_bwd.  gamma, beta may be None."""
+    graph); mean, rstd: (graphs, groups), written for group_norm_bwd.  gamma, beta may be None.
+    max_seg: rows of the longest graph, where the program knows it: without it (-1) a batch of small
+    graphs takes up to twice as long, here and in group_norm_bwd."""
     dev = _device_of(X)
     n, c = X.shape
     k, seg = _segments(seg_ptr, dev)
@@ -577,7 +579,7 @@ def group_norm_bwd(X, dY, mean, rstd, groups, gamma, beta, dX=None, dgamma=None,
                    max_seg=-1, act=ACT_NONE, ws: _Workspace | None = None, stream=None):
     """Gradients of group_norm from dY = dLoss/dout, with the mean and rstd it wrote
     (gcn_group_norm_bwd): dX (may be dY), dgamma, dbeta; each may be None.  mean and rstd may have
-    rows or columns apart (slices, transposed results): such a one is copied first."""
+    rows or columns apart (slices, transposed results): such a one is copied first.  max_seg as there."""
     dev = _device_of(X)
     n, c = X.shape
     k, seg = _segments(seg_ptr, dev)
