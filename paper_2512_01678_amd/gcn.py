@@ -2,7 +2,8 @@
 
 Argument marshalling only: every computation runs in the HIP library.  torch
 supplies device memory (tensor.data_ptr()) and the HIP stream
-(torch.cuda.current_stream().cuda_stream); nothing here computes on tensors.
+(torch.cuda.current_stream().cuda_stream); nothing here computes on tensors (a
+statistic whose rows or columns lie apart is copied).
 If libgcn.so is missing, importing this module raises: there is no fallback.
 """
 from __future__ import annotations
